@@ -17,20 +17,24 @@ __device__ __forceinline__ float f8_scale(float amax) { return __fdiv_rn(fmaxf(a
 // two values (packed pairs) instead of a division each; scales near the ends of the
 // exponent range, where a residual could underflow, take the division.
 struct F8Divider {
-  float s;
+  float s0, s1;        // of the first and the second of two values
   uint64_t r2, ns2;
   bool plain;
-  __device__ __forceinline__ explicit F8Divider(float scale) : s(scale), plain(!(scale > 0x1p-60f && scale < 0x1p60f)) {
-    const float r = 1.f / scale;
-    r2 = ptx::pack2(r, r);
-    ns2 = ptx::pack2(-scale, -scale);
-  }
+  // r0, r1: 1 / s0, 1 / s1, rounded.
+  __device__ __forceinline__ F8Divider(float a, float b, float r0, float r1)
+      : s0(a), s1(b), r2(ptx::pack2(r0, r1)), ns2(ptx::pack2(-a, -b)),
+        plain(!(fminf(a, b) > 0x1p-60f && fmaxf(a, b) < 0x1p60f)) {}
+  __device__ __forceinline__ F8Divider(float s, float r) : F8Divider(s, s, r, r) {}
+  __device__ __forceinline__ explicit F8Divider(float s) : F8Divider(s, 1.f / s) {}
   // Two quotients; not for `plain`.
   __device__ __forceinline__ float2 operator()(float a, float b) const {
     const uint64_t x = ptx::pack2(a, b);
     uint64_t q = ptx::mul2(x, r2);
     q = ptx::fma2(ptx::fma2(q, ns2, x), r2, q);
     return ptx::unpack2(ptx::fma2(ptx::fma2(q, ns2, x), r2, q));
+  }
+  __device__ __forceinline__ float2 slow(float a, float b) const {
+    return make_float2(__fdiv_rn(a, s0), __fdiv_rn(b, s1));
   }
 };
 
@@ -56,8 +60,7 @@ __device__ __forceinline__ void f8_quantise(const float (&v)[kN], const F8Divide
   if (div.plain) {
 #pragma unroll
     for (int j = 0; j < kN / 4; ++j)
-      w[j] = f8_pack2(make_float2(__fdiv_rn(v[4 * j], div.s), __fdiv_rn(v[4 * j + 1], div.s))) |
-             f8_pack2(make_float2(__fdiv_rn(v[4 * j + 2], div.s), __fdiv_rn(v[4 * j + 3], div.s))) << 16;
+      w[j] = f8_pack2(div.slow(v[4 * j], v[4 * j + 1])) | f8_pack2(div.slow(v[4 * j + 2], v[4 * j + 3])) << 16;
   } else {
 #pragma unroll
     for (int j = 0; j < kN / 4; ++j)

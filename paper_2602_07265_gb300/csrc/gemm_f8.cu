@@ -571,16 +571,16 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
         }
         m = fmaxf(m, s_amax[(side + 1 - half) * 128 + row]);
         if (live) {
-          // h carries fp32 rounding itself, so the quotient may too: one product with 448 / amax.
-          const float s = f8_scale(m), r = 1.f / s;
+          const float s = f8_scale(m);
+          const F8Divider div(s);
           uint8_t *dst = p.hq + out_row * p.N + t.cb * 128 + half * 64;
 #pragma unroll
           for (int c = 0; c < 64; c += 32) {
-            uint32_t w[8];
+            float part[32];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              w[j] = f8_pack2(make_float2(h[c + 4 * j] * r, h[c + 4 * j + 1] * r)) |
-                     f8_pack2(make_float2(h[c + 4 * j + 2] * r, h[c + 4 * j + 3] * r)) << 16;
+            for (int j = 0; j < 32; ++j) part[j] = h[c + j];
+            uint32_t w[8];
+            f8_quantise<32>(part, div, w);
             store32(dst + c, w);
           }
           if (half == 0) p.hs[out_row * p.NB + t.cb] = s;

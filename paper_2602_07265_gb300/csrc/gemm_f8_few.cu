@@ -547,15 +547,22 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
         const float s = f8_scale(m), r = 1.f / s;
         const int tok0 = g * kHalf;
         if (ok) {
-          // h carries fp32 rounding itself, so the quotient may too: one product with 1 / s.
           uint8_t *dst = p.hq + static_cast<size_t>(t.row0 + tok0) * p.N + t.cb * 128 + row;
+          // Every token has a scale of its own, in lane j.
+          auto quantise = [&](auto quotients) {
 #pragma unroll
-          for (int j = 0; j < kHalf; j += 2) {
-            const uint32_t two = f8_pack2(make_float2(h[j] * __shfl_sync(0xffffffffu, r, j),
-                                                      h[j + 1] * __shfl_sync(0xffffffffu, r, j + 1)));
-            if (tok0 + j < t.ntok) dst[static_cast<size_t>(j) * p.N] = static_cast<uint8_t>(two);
-            if (tok0 + j + 1 < t.ntok) dst[static_cast<size_t>(j + 1) * p.N] = static_cast<uint8_t>(two >> 8);
-          }
+            for (int j = 0; j < kHalf; j += 2) {
+              auto of = [&](float v, int k) { return __shfl_sync(0xffffffffu, v, k); };
+              const F8Divider div(of(s, j), of(s, j + 1), of(r, j), of(r, j + 1));
+              const uint32_t two = f8_pack2(quotients(div, h[j], h[j + 1]));
+              if (tok0 + j < t.ntok) dst[static_cast<size_t>(j) * p.N] = static_cast<uint8_t>(two);
+              if (tok0 + j + 1 < t.ntok) dst[static_cast<size_t>(j + 1) * p.N] = static_cast<uint8_t>(two >> 8);
+            }
+          };
+          if (__any_sync(0xffffffffu, lane < kHalf && F8Divider(s, r).plain))
+            quantise([](const F8Divider &div, float a, float b) { return div.slow(a, b); });
+          else
+            quantise([](const F8Divider &div, float a, float b) { return div(a, b); });
           if (q == 0 && lane < kHalf && tok0 + lane < t.ntok)
             p.hs[static_cast<size_t>(t.row0 + tok0 + lane) * p.NB + t.cb] = s;
         }
