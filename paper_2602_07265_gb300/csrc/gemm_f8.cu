@@ -56,7 +56,6 @@ constexpr int kCols = 256;                       // weight rows of a unit, TMEM 
 constexpr int kRows = 128;                       // token rows of one CTA
 constexpr int kABytes = kRows * kBK;             // 16 KB of tokens
 constexpr int kBoxes = 4;                        // token boxes of 16, 32, 64, 128 rows
-constexpr uint64_t kWaitNs = 1000000000ull;      // 1 s per wait
 
 constexpr int kBBytes = kCols / 2 * kBK;          // this CTA's weights of a K block: 16 KB
 constexpr int kStageBytes = kABytes + kBBytes;
@@ -88,6 +87,8 @@ struct F8Params {
   int rows, N, KB, NB;     // NB: scale rows of a matrix, ceil(N / 128)
   int edge;                // box rows of a matrix's last 128-row block, if that is not whole
   int early;
+  uint32_t hold;           // see F8Args
+  uint64_t wait_ns;
 };
 
 __device__ __forceinline__ void convert(float v, float *o) { *o = v; }
@@ -367,6 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
   if (warp < 4) regs_dec<kIssueRegs>();
   if (warp == 0) {
     // ------------------------------------------------ TMA producer
+    const uint32_t hold = blockIdx.x == 0 ? p.hold : 0;
     int stage = 0, kb = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -376,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
 #pragma unroll 1
     for (uint32_t i = 0; i < n_blocks; ++i) {
       if (i >= kStages) {
-        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, kWaitNs, abort_flag);
+        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.wait_ns, abort_flag);
         if (!ok) break;
       }
       if (elect_one()) {
@@ -384,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
           if (rank == 0) mbar_arrive_expect_tx(full_bar(stage), step_bytes(t));
           load_b(t, kb, stage);
         }
-        load_a(t, kb, stage);
+        if (i + 1 != hold) load_a(t, kb, stage);
       }
       __syncwarp();
       if (++kb == KB && i + 1 < n_blocks) {
@@ -401,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
     if (n_blocks > 0)
       for (int j = 0; ok && j < kStages; ++j) {
         if (n_blocks + j >= static_cast<uint32_t>(kStages))
-          ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, kWaitNs, abort_flag);
+          ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.wait_ns, abort_flag);
         if (++stage == kStages) {
           stage = 0;
           phase ^= 1u;
@@ -424,12 +426,12 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
     bool ok = true;
 #pragma unroll 1
     for (uint32_t i = 0; i < n_blocks; ++i) {
-      ok = mbar_wait_warp(full_bar(stage), phase, kWaitNs, abort_flag);
+      ok = mbar_wait_warp(full_bar(stage), phase, p.wait_ns, abort_flag);
       if (!ok) break;
       const uint64_t da = desc0 + static_cast<uint64_t>(stage * (kStageBytes >> 4));
       const uint32_t turn = i & 1u;
       const int b = 2 * g + static_cast<int>(turn);
-      ok = mbar_wait_warp(accempty_bar(b), ((i >> 1) & 1u) ^ 1u, kWaitNs, abort_flag);
+      ok = mbar_wait_warp(accempty_bar(b), ((i >> 1) & 1u) ^ 1u, p.wait_ns, abort_flag);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
@@ -455,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
     if (n_blocks > 0) {
       if (elect_one()) mma_commit_pair_local(drain_bar);
       volatile int no_abort = 0;
-      mbar_wait_warp(drain_bar, 0, kWaitNs, &no_abort);
+      mbar_wait_warp(drain_bar, 0, kF8WaitNs, &no_abort);
     }
   } else if (warp >= 4) {
     // ------------------------------------------------ epilogue
@@ -472,7 +474,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
     auto meet = [&]() {
       __syncwarp();
       if (lane == 0) mbar_arrive(meet_bar);
-      return mbar_wait_warp(meet_bar, met++ & 1u, kWaitNs, abort_flag);
+      return mbar_wait_warp(meet_bar, met++ & 1u, p.wait_ns, abort_flag);
     };
     uint32_t i = 0;
     int u = u_first;
@@ -516,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
           b0_next = __ldg(weight_scale(next, 0));
           b1_next = __ldg(weight_scale(next, 1));
         }
-        ok = mbar_wait_warp(accfull0 + 8u * turn, (i >> 1) & 1u, kWaitNs, abort_flag);
+        ok = mbar_wait_warp(accfull0 + 8u * turn, (i >> 1) & 1u, p.wait_ns, abort_flag);
         if (!ok) break;
         tc_fence_after();
         auto release = [&]() {
@@ -705,6 +707,8 @@ cudaError_t launch(const F8Args &a, cudaStream_t s) {
   p.KB = (a.K + kBK - 1) / kBK;
   p.NB = (a.N + 127) / 128;
   p.early = a.early;
+  p.hold = a.hold;
+  p.wait_ns = a.wait_ns;
   const long long tiles = a.tiles != nullptr ? a.max_tiles : (a.rows + kF8PairTile - 1) / kF8PairTile;
   const long long units = tiles * (kGlu ? p.NB : (a.N + kCols - 1) / kCols);
   const int sms = a.n_sms < kF8Ctas ? a.n_sms : kF8Ctas;

@@ -59,7 +59,6 @@ constexpr int kWBytes = kRows * kBK;             // 32 KB of weights per K block
 constexpr int kBufs = 4;                         // TMEM buffers
 constexpr int kBoxes = 3;                        // token boxes of 16, 32, 64 rows
 constexpr int kMinBlocks = 2;                    // K blocks per CTA at least
-constexpr uint64_t kWaitNs = 1000000000ull;      // 1 s per wait
 
 template <int kTok, bool kSplit>
 struct Shape {
@@ -88,6 +87,8 @@ struct FewParams {
   int rows, N, KB, NB;     // NB: scale rows of a matrix, ceil(N / 128)
   int edge;                // box rows of a matrix's last 128-row block, if that is not whole
   int early;
+  uint32_t hold;           // see F8Args
+  uint64_t wait_ns;
 };
 
 __device__ __forceinline__ void convert(float v, float *o) { *o = v; }
@@ -254,6 +255,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
   if (warp < 4) regs_dec<kIssueRegs>();
   if (warp == 0) {
     // ------------------------------------------------ TMA producer
+    const uint32_t hold = blockIdx.x == 0 ? p.hold : 0;
     int stage = 0, kb = kb_first, u = u_first;
     uint32_t phase = 0;
     bool ok = true;
@@ -262,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
 #pragma unroll 1
     for (uint32_t i = 0; i < n_blocks; ++i) {
       if (i >= kStages) {
-        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, kWaitNs, abort_flag);
+        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.wait_ns, abort_flag);
         if (!ok) break;
       }
       if (elect_one()) {
@@ -270,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
           mbar_arrive_expect_tx(full_bar(stage), step_bytes(t));
           load_w(t, kb, stage);
         }
-        load_x(t, kb, stage);
+        if (i + 1 != hold) load_x(t, kb, stage);
       }
       __syncwarp();
       if (++kb == kb_end && i + 1 < n_blocks) {
@@ -283,13 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
         phase ^= 1u;
       }
     }
-    if (!ok) {
-      if (lane == 0) fail();
-      // Copies may be in flight whose barrier no longer completes: they land
-      // in microseconds; stay for two milliseconds.
-      const uint64_t t_end = globaltimer() + 2000000ull;
-      while (globaltimer() < t_end) __nanosleep(1000);
-    }
+    if (!ok && lane == 0) fail();
   } else if (warp == 1) {
     // ------------------------------------------------ MMA issuer
     const uint64_t desc0 = sw128_desc(__shfl_sync(0xffffffffu, sbase, 0));
@@ -304,8 +300,8 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
         idesc = __shfl_sync(0xffffffffu, idesc_e4m3(128, 16 << box_of(t.ntok)), 0);
       }
       const int buf = static_cast<int>(i % kBufs);
-      ok = mbar_wait_warp(accempty_bar(buf), ((i / kBufs) & 1u) ^ 1u, kWaitNs, abort_flag) &&
-           mbar_wait_warp(full_bar(stage), phase, kWaitNs, abort_flag);
+      ok = mbar_wait_warp(accempty_bar(buf), ((i / kBufs) & 1u) ^ 1u, p.wait_ns, abort_flag) &&
+           mbar_wait_warp(full_bar(stage), phase, p.wait_ns, abort_flag);
       if (!ok) break;
       tc_fence_after();
       const uint64_t dw = desc0 + static_cast<uint64_t>(stage * (kStageBytes >> 4)), dx = dw + (kWBytes >> 4);
@@ -335,7 +331,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
     if (n_blocks > 0) {
       if (elect_one()) mma_commit(drain_bar);
       volatile int no_abort = 0;
-      mbar_wait_warp(drain_bar, 0, kWaitNs, &no_abort);
+      mbar_wait_warp(drain_bar, 0, kF8WaitNs, &no_abort);
     }
   } else if (warp >= 4) {
     // ------------------------------------------------ epilogue
@@ -351,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
     auto meet = [&]() {
       __syncwarp();
       if (lane == 0) mbar_arrive(meet_bar);
-      return mbar_wait_warp(meet_bar, met++ & 1u, kWaitNs, abort_flag);
+      return mbar_wait_warp(meet_bar, met++ & 1u, p.wait_ns, abort_flag);
     };
     uint32_t i = 0;
     int u = u_first;
@@ -383,7 +379,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
           if (kTok > 32) a1 = token_scale(lane + 32, kb + 1);
           b = __ldg(sb + kb + 1);
         }
-        ok = mbar_wait_warp(accfull_bar(buf), (i / kBufs) & 1u, kWaitNs, abort_flag);
+        ok = mbar_wait_warp(accfull_bar(buf), (i / kBufs) & 1u, p.wait_ns, abort_flag);
         if (!ok) break;
         tc_fence_after();
         const uint32_t tb = tq + buf * 2 * kTok;
@@ -472,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
           if (lane == 0) mbar_arrive_cluster(map_to_rank(parts_bar, 0));
           finish = false;
         } else if (ok) {
-          ok = mbar_wait_cluster(parts_bar, 0, kWaitNs, abort_flag);
+          ok = mbar_wait_cluster(parts_bar, 0, p.wait_ns, abort_flag);
           const uint32_t src = smem_u32(s_swap + g * 128 + row);
           if (ok)
             add_parts(1, ranks - 1,
@@ -588,6 +584,12 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
 
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag) {
+    // Copies may be in flight whose barrier nobody has waited for (the producer's last ones are the MMA
+    // issuer's to wait for): they land in microseconds; stay for two milliseconds.
+    const uint64_t t_end = globaltimer() + 2000000ull;
+    while (globaltimer() < t_end) __nanosleep(1000);
+  }
   if (kSplit) cluster_sync();   // none leaves while another may still read its sums or signal it
   if (warp == 1) {
     tc_fence_after();
@@ -647,6 +649,8 @@ cudaError_t launch(const F8Args &a, cudaStream_t s) {
   p.KB = (a.K + kBK - 1) / kBK;
   p.NB = (a.N + 127) / 128;
   p.early = a.early;
+  p.hold = a.hold;
+  p.wait_ns = a.wait_ns;
   const long long tiles = a.tiles != nullptr ? a.max_tiles : (a.rows + kTok - 1) / kTok;
   const long long units = tiles * (kGlu ? p.NB : (a.N + kRows - 1) / kRows);
   const int sms = a.n_sms < kF8Ctas ? a.n_sms : kF8Ctas;

@@ -14,6 +14,7 @@ constexpr int kF8PairTile = 256;     // token rows of a tile on CTA pairs
 constexpr int kF8FewTile = 64;       // and at most in the form for few rows
 constexpr int kF8Ctas = 152;         // CTAs of a float8 product at most (one per SM)
 constexpr int kF8CutBlocks = 8;      // K blocks per CTA that sharing units has to save: joining costs about 5 us
+constexpr uint64_t kF8WaitNs = 1000000000ull;   // 1 s per wait inside a product
 constexpr int kF8Regs = 168;         // registers per thread of the product kernels at their launch
 constexpr float kTinyAmax = 7.8886090522101181e-31f;   // 2^-100
 constexpr float kE4m3Max = 448.f;
@@ -111,6 +112,8 @@ struct F8Args {
   int n_sms;
   float *part;                 // few rows: f8_part_bytes(), partial sums of cut units
   int32_t *cnt;                // and [kF8Ctas] arrivals, zero at the start
+  uint64_t wait_ns;            // limit of a wait; 0: kF8WaitNs
+  uint32_t hold;               // self-test: CTA 0 never loads the tokens of its K block hold - 1; 0: loads all
 };
 // The product kernels are launched with 168 registers for each of their 384 threads and hand
 // them out again by warpgroup.  A split that asks for more than the launch holds would wait for
@@ -134,7 +137,10 @@ size_t f8_part_bytes();
 int f8_split(int tile_tok, long long units, int K);
 cudaError_t launch_f8_pairs(const F8Args &a, cudaStream_t s);   // gemm_f8.cu
 cudaError_t launch_f8_few(const F8Args &a, cudaStream_t s);     // gemm_f8_few.cu
-inline cudaError_t launch_f8(const F8Args &a, cudaStream_t s) {
+// Sets wait_ns, and hold for the launch that xshare_selftest_f8_hold() has named (selftest.cu).
+void f8_waits(F8Args *a);
+inline cudaError_t launch_f8(F8Args a, cudaStream_t s) {
+  f8_waits(&a);
   return a.tile_tok == kF8PairTile ? launch_f8_pairs(a, s) : launch_f8_few(a, s);
 }
 

@@ -6,8 +6,13 @@
 // XS_DEV_TIMEOUT in the caller's xs_stats and return, and the CUDA context
 // must stay usable.  A second wait runs out for half of the warp's lanes only:
 // all of them must be told so.  No fault, trap or unbounded loop is involved.
+//
+// The waits of the float8 products are made to run out in the products themselves:
+// one CTA leaves out one load, with a short limit, so that the kernels' own way
+// out is what runs.
 #include <cuda_runtime.h>
 
+#include "ops_internal.cuh"
 #include "tc_ptx.cuh"
 #include "xs_internal.cuh"
 
@@ -52,8 +57,35 @@ __global__ void wait_timeout_kernel(xs_stats *stats, unsigned long long budget_n
   }
 }
 
+// Set by this host thread for a product that it launches later.
+struct Hold {
+  int launches = -1;   // products before it; -1: none
+  uint32_t block = 0;
+  uint64_t wait_ns = 0;
+};
+thread_local Hold t_hold;
+
 }  // namespace
+
+void f8_waits(F8Args *a) {
+  a->wait_ns = kF8WaitNs;
+  if (t_hold.launches < 0 || t_hold.launches-- > 0) return;
+  a->wait_ns = t_hold.wait_ns;
+  a->hold = t_hold.block + 1;
+}
+
 }  // namespace xs
+
+// For tests: of the float8 products that this host thread launches from now on, the one after
+// `launches` others waits at most wait_ns at a time, and its CTA 0 leaves out the tokens
+// of its K block `block` (ends without the timeout if it has none).
+extern "C" int xshare_selftest_f8_hold(int launches, uint32_t block, uint64_t wait_ns) {
+  if (launches < 0 || block > 1u << 30 || wait_ns == 0 || wait_ns > xs::kF8WaitNs) return XS_ERR_PARAM;
+  xs::t_hold.launches = launches;
+  xs::t_hold.block = block;
+  xs::t_hold.wait_ns = wait_ns;
+  return XS_OK;
+}
 
 extern "C" int xshare_selftest_wait_timeout(xs_stats *stats, uint64_t budget_ns,
                                             xs_stream_t stream) {
