@@ -25,6 +25,8 @@
  * is large enough for some sizes is so for smaller ones.  Every call gives the same
  * bits for the same arguments; how a float8 product groups its sums over K
  * depends on the number of rows, so a row's last bits may change with its company.
+ * A wait inside a product that runs out is reported in stats->status where stats is given; in
+ * any case the part of the output that the product could not finish is NaN (and more may be).
  * The library serves: nothing here has a backward pass.
  *
  * 8-bit floating point is e4m3 (finite values up to 448, NaN, no infinity), one

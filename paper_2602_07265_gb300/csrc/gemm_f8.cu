@@ -35,6 +35,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <cmath>
 #include <cstring>
 #include <type_traits>
 
@@ -229,6 +230,30 @@ __device__ __forceinline__ void store_row16(const CUtensorMap *tm, uint32_t stag
 template <class T, bool kWide>
 using ShapeOf = Shape<std::is_same_v<T, Rows16> ? 4096 : kWide ? 0 : kOddOut>;
 
+// The units of a CTA pair in which a wait ran out become NaN, those that it had finished too, so that a
+// call without `stats` does not pass for a whole one.
+template <bool kGlu, class T>
+__device__ __noinline__ void give_nan(const F8Params &p, int n_units) {
+  using Out = std::conditional_t<std::is_same_v<T, Rows16>, __half, T>;
+  const int w = static_cast<int>(threadIdx.x >> 5) - 4, half = w >> 2;
+  const int trow = (w & 3) * 32 + static_cast<int>(threadIdx.x & 31) + static_cast<int>(cluster_ctarank()) * kRows;
+  const int CB = kGlu ? p.NB : (p.N + kCols - 1) / kCols;
+  for (int u = static_cast<int>(blockIdx.x >> 1); u < n_units; u += static_cast<int>(gridDim.x >> 1)) {
+    const int i = u / CB, cb = u - i * CB;
+    const int row0 = p.tiles != nullptr ? p.tiles[i].row0 : i * kF8PairTile;
+    const int ntok = p.tiles != nullptr ? p.tiles[i].ntok : min(kF8PairTile, p.rows - row0);
+    if (trow >= ntok) continue;
+    const size_t at = static_cast<size_t>(row0 + trow) * p.N;
+    for (int c = 0; c < (kGlu ? 64 : 128); ++c) {
+      const int n = (kGlu ? cb * 128 : cb * kCols) + half * 64 + (c & 63) + (c >> 6) * 128;
+      if constexpr (kGlu)
+        p.hq[at + n] = kE4m3Nan;
+      else if (n < p.N)
+        convert(NAN, static_cast<Out *>(p.y) + at + n);
+    }
+  }
+}
+
 // T: the output's type (unused in the SwiGLU form); kWide: store_row() serves.  (An instance
 // with both ways to store spilled registers in the loop over K.)
 template <bool kGlu, class T, bool kWide>
@@ -283,6 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
   const int n_tiles = listed ? __ldcg(&p.meta->n_tiles) : (p.rows + kF8PairTile - 1) / kF8PairTile;
   const int CB = kGlu ? p.NB : (p.N + kCols - 1) / kCols, KB = p.KB;
   const int n_units = n_tiles * CB;   // below 2^26 within the limits of the calls
+  if (threadIdx.x == 0) tmem_slot[2] = static_cast<uint32_t>(n_units);   // for give_nan()
   struct Unit {
     int expert, row0, ntok, cb;
   };
@@ -378,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
 #pragma unroll 1
     for (uint32_t i = 0; i < n_blocks; ++i) {
       if (i >= kStages) {
-        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.wait_ns, abort_flag);
+        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, kF8WaitNs, abort_flag);
         if (!ok) break;
       }
       if (elect_one()) {
@@ -403,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
     if (n_blocks > 0)
       for (int j = 0; ok && j < kStages; ++j) {
         if (n_blocks + j >= static_cast<uint32_t>(kStages))
-          ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.wait_ns, abort_flag);
+          ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, kF8WaitNs, abort_flag);
         if (++stage == kStages) {
           stage = 0;
           phase ^= 1u;
@@ -431,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
       const uint64_t da = desc0 + static_cast<uint64_t>(stage * (kStageBytes >> 4));
       const uint32_t turn = i & 1u;
       const int b = 2 * g + static_cast<int>(turn);
-      ok = mbar_wait_warp(accempty_bar(b), ((i >> 1) & 1u) ^ 1u, p.wait_ns, abort_flag);
+      ok = mbar_wait_warp(accempty_bar(b), ((i >> 1) & 1u) ^ 1u, kF8WaitNs, abort_flag);
       if (!ok) break;
       tc_fence_after();
       if (elect_one()) {
@@ -474,7 +500,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
     auto meet = [&]() {
       __syncwarp();
       if (lane == 0) mbar_arrive(meet_bar);
-      return mbar_wait_warp(meet_bar, met++ & 1u, p.wait_ns, abort_flag);
+      return mbar_wait_warp(meet_bar, met++ & 1u, kF8WaitNs, abort_flag);
     };
     uint32_t i = 0;
     int u = u_first;
@@ -518,7 +544,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
           b0_next = __ldg(weight_scale(next, 0));
           b1_next = __ldg(weight_scale(next, 1));
         }
-        ok = mbar_wait_warp(accfull0 + 8u * turn, (i >> 1) & 1u, p.wait_ns, abort_flag);
+        ok = mbar_wait_warp(accfull0 + 8u * turn, (i >> 1) & 1u, kF8WaitNs, abort_flag);
         if (!ok) break;
         tc_fence_after();
         auto release = [&]() {
@@ -619,6 +645,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
 
   tc_fence_before();
   __syncthreads();
+  if (*abort_flag && warp >= 4) give_nan<kGlu, T>(p, static_cast<int>(tmem_slot[2]));
   cluster_sync();   // neither CTA leaves while the other may still signal it
   if (warp == 1) {
     tc_fence_after();

@@ -34,6 +34,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <cmath>
 #include <cstring>
 #include <type_traits>
 
@@ -94,6 +95,30 @@ struct FewParams {
 __device__ __forceinline__ void convert(float v, float *o) { *o = v; }
 __device__ __forceinline__ void convert(float v, __nv_bfloat16 *o) { *o = __float2bfloat16_rn(v); }
 __device__ __forceinline__ void convert(float v, __half *o) { *o = __float2half_rn(v); }
+
+// The units of a CTA in which a wait ran out become NaN, those that it had finished too, so that a
+// call without `stats` does not pass for a whole one.  (A cut unit without this CTA's part is
+// finished by nobody else; all CTAs of a cluster give up together.)  `mine`: the first unit, the end, the step.
+template <int kTok, bool kGlu, class T>
+__device__ __noinline__ void give_nan(const FewParams &p, const uint32_t *mine) {
+  const int w = static_cast<int>(threadIdx.x >> 5) - 4, g = w >> 2, row = (w & 3) * 32 + static_cast<int>(threadIdx.x & 31);
+  const int CB = kGlu ? p.NB : (p.N + kRows - 1) / kRows;
+  for (uint32_t v = mine[0]; v < mine[1]; v += mine[2]) {
+    const int u = static_cast<int>(v);
+    const int i = u / CB, cb = u - i * CB;
+    const int row0 = p.tiles != nullptr ? p.tiles[i].row0 : i * kTok;
+    const int ntok = p.tiles != nullptr ? p.tiles[i].ntok : min(kTok, p.rows - row0);
+    const int n = kGlu ? cb * 128 + row : cb * kRows + g * 128 + row;
+    const int j0 = kGlu ? g * (kTok / 2) : 0, j1 = kGlu ? min(ntok, j0 + kTok / 2) : ntok;
+    for (int j = j0; j < j1 && n < p.N; ++j) {
+      const size_t at = static_cast<size_t>(row0 + j) * p.N + n;
+      if constexpr (kGlu)
+        p.hq[at] = kE4m3Nan;
+      else
+        convert(NAN, static_cast<T *>(p.y) + at);
+    }
+  }
+}
 
 // T: the output's type (unused in the SwiGLU form).  kSplit: launched as a cluster for every unit.
 template <int kTok, bool kGlu, class T, bool kSplit>
@@ -178,6 +203,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
   uint32_t n_blocks =
       u_first < n_units ? static_cast<uint32_t>((n_units - u_first + unit_step - 1) / unit_step) * (kb_end - kb_begin) : 0;
   uint32_t n_cta = 1;    // CTAs that share the blocks, if units are cut
+  int n_mine = n_units;  // units from here on are other CTAs'
   if (!kSplit) {
     // What a CTA does at most with whole units, and with equal shares.
     const long long whole = static_cast<long long>((n_units + unit_step - 1) / unit_step) * KB;
@@ -189,8 +215,15 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
       u_first = static_cast<int>(first / KB);
       kb_first = static_cast<int>(first - static_cast<long long>(u_first) * KB);
       n_blocks = static_cast<uint32_t>(last - first);
+      n_mine = static_cast<int>((last + KB - 1) / KB);
       unit_step = 1;
     }
+  }
+
+  if (threadIdx.x == 0) {   // for give_nan()
+    tmem_slot[5] = static_cast<uint32_t>(u_first);
+    tmem_slot[6] = static_cast<uint32_t>(n_mine);
+    tmem_slot[7] = static_cast<uint32_t>(unit_step);
   }
 
   auto box_of = [](int n) { return n <= 16 ? 0 : n <= 32 ? 1 : 2; };
@@ -264,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
 #pragma unroll 1
     for (uint32_t i = 0; i < n_blocks; ++i) {
       if (i >= kStages) {
-        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, p.wait_ns, abort_flag);
+        ok = mbar_wait_warp(empty_bar(stage), phase ^ 1u, kF8WaitNs, abort_flag);
         if (!ok) break;
       }
       if (elect_one()) {
@@ -300,7 +333,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
         idesc = __shfl_sync(0xffffffffu, idesc_e4m3(128, 16 << box_of(t.ntok)), 0);
       }
       const int buf = static_cast<int>(i % kBufs);
-      ok = mbar_wait_warp(accempty_bar(buf), ((i / kBufs) & 1u) ^ 1u, p.wait_ns, abort_flag) &&
+      ok = mbar_wait_warp(accempty_bar(buf), ((i / kBufs) & 1u) ^ 1u, kF8WaitNs, abort_flag) &&
            mbar_wait_warp(full_bar(stage), phase, p.wait_ns, abort_flag);
       if (!ok) break;
       tc_fence_after();
@@ -347,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
     auto meet = [&]() {
       __syncwarp();
       if (lane == 0) mbar_arrive(meet_bar);
-      return mbar_wait_warp(meet_bar, met++ & 1u, p.wait_ns, abort_flag);
+      return mbar_wait_warp(meet_bar, met++ & 1u, kF8WaitNs, abort_flag);
     };
     uint32_t i = 0;
     int u = u_first;
@@ -379,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
           if (kTok > 32) a1 = token_scale(lane + 32, kb + 1);
           b = __ldg(sb + kb + 1);
         }
-        ok = mbar_wait_warp(accfull_bar(buf), (i / kBufs) & 1u, p.wait_ns, abort_flag);
+        ok = mbar_wait_warp(accfull_bar(buf), (i / kBufs) & 1u, kF8WaitNs, abort_flag);
         if (!ok) break;
         tc_fence_after();
         const uint32_t tb = tq + buf * 2 * kTok;
@@ -468,7 +501,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
           if (lane == 0) mbar_arrive_cluster(map_to_rank(parts_bar, 0));
           finish = false;
         } else if (ok) {
-          ok = mbar_wait_cluster(parts_bar, 0, p.wait_ns, abort_flag);
+          ok = mbar_wait_cluster(parts_bar, 0, kF8WaitNs, abort_flag);
           const uint32_t src = smem_u32(s_swap + g * 128 + row);
           if (ok)
             add_parts(1, ranks - 1,
@@ -589,6 +622,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
     // issuer's to wait for): they land in microseconds; stay for two milliseconds.
     const uint64_t t_end = globaltimer() + 2000000ull;
     while (globaltimer() < t_end) __nanosleep(1000);
+    if (warp >= 4) give_nan<kTok, kGlu, T>(p, tmem_slot + 5);
   }
   if (kSplit) cluster_sync();   // none leaves while another may still read its sums or signal it
   if (warp == 1) {

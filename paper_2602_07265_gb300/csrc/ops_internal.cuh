@@ -18,6 +18,7 @@ constexpr uint64_t kF8WaitNs = 1000000000ull;   // 1 s per wait inside a product
 constexpr int kF8Regs = 168;         // registers per thread of the product kernels at their launch
 constexpr float kTinyAmax = 7.8886090522101181e-31f;   // 2^-100
 constexpr float kE4m3Max = 448.f;
+constexpr uint8_t kE4m3Nan = 0x7f;
 
 // Facts of one permutation, read by the kernels after it.
 struct PermMeta {
@@ -112,7 +113,7 @@ struct F8Args {
   int n_sms;
   float *part;                 // few rows: f8_part_bytes(), partial sums of cut units
   int32_t *cnt;                // and [kF8Ctas] arrivals, zero at the start
-  uint64_t wait_ns;            // limit of a wait; 0: kF8WaitNs
+  uint64_t wait_ns;            // limit of the MMA issuers' waits for operands (the others': kF8WaitNs)
   uint32_t hold;               // self-test: CTA 0 never loads the tokens of its K block hold - 1; 0: loads all
 };
 // The product kernels are launched with 168 registers for each of their 384 threads and hand

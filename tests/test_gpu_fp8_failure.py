@@ -97,3 +97,46 @@ def test_experts_report_and_the_next_are_right(ops, B, n, k, d, F, which):
     assert st[5].item() == TIMEOUT
     ops.xshare_experts_fp8(x, ids, w, ex, y, work, stats=st)
     assert st[5].item() == OK and torch.equal(y, want)
+
+
+def owed(y, want):
+    """Elements that are NaN; all others have to be those of a whole call."""
+    gone = torch.isnan(y)
+    assert gone.any() and torch.equal(torch.where(gone, want, y), want)
+    return gone
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("stats", [False, True])
+@pytest.mark.parametrize("M,N,K,E,block", PRODUCTS)
+def test_what_a_product_could_not_finish_is_nan(ops, M, N, K, E, block, stats, dtype):
+    """With and without statistics: no element keeps what the buffer held before."""
+    q, s = rows_of(ops, randn(M, K, seed=11))
+    w, ws = blocks_of(ops, randn(E, N, K, seed=12, std=0.02))
+    off = torch.linspace(0, M, E + 1).int().to(DEV) if E > 1 else None
+    work = torch.empty(ops.xshare_matmul_fp8_workspace_size(M, N, K, E), dtype=torch.uint8, device=DEV)
+    st = torch.zeros(8, dtype=torch.int32, device=DEV) if stats else None
+    want, y = torch.empty(M, N, dtype=dtype, device=DEV), torch.full((M, N), 333.0, dtype=dtype, device=DEV)
+    ops.xshare_matmul_fp8(q, s, w, ws, want, work, offsets=off, stats=st)
+    assert not torch.isnan(want).any()
+    hold(ops, 0, block)
+    ops.xshare_matmul_fp8(q, s, w, ws, y, work, offsets=off, stats=st)
+    owed(y, want)
+
+
+@pytest.mark.parametrize("which", [0, 1])
+@pytest.mark.parametrize("B,n,k,d,F", EXPERTS)
+def test_what_the_experts_could_not_finish_is_nan(ops, B, n, k, d, F, which):
+    ex = ops.Fp8Experts.quantise(randn(n, F, d, seed=13, std=0.05), randn(n, F, d, seed=14, std=0.05),
+                                 randn(n, d, F, seed=15, std=0.05))
+    x = randn(B, d, seed=16)
+    ids = torch.rand(B, n, generator=torch.Generator().manual_seed(17)).argsort(1)[:, :k].int().contiguous().to(DEV)
+    w = torch.full((B, k), 1.0 / k, device=DEV)
+    work = torch.empty(ops.xshare_experts_fp8_workspace_size(B, n, k, d, F), dtype=torch.uint8, device=DEV)
+    want, y = torch.empty_like(x), torch.full_like(x, 333.0)
+    ops.xshare_experts_fp8(x, ids, w, ex, want, work)
+    hold(ops, which, 1)
+    ops.xshare_experts_fp8(x, ids, w, ex, y, work)
+    gone = owed(y, want)
+    if which == 0:   # an activation that is missing takes the token's whole row with it
+        assert torch.equal(gone.any(1), gone.all(1))
