@@ -581,10 +581,11 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
           auto quantise = [&](auto quotients) {
 #pragma unroll
             for (int j = 0; j < kHalf; j += 2) {
+              if (tok0 + j >= t.ntok) break;
               auto of = [&](float v, int k) { return __shfl_sync(0xffffffffu, v, k); };
               const F8Divider div(of(s, j), of(s, j + 1), of(r, j), of(r, j + 1));
               const uint32_t two = f8_pack2(quotients(div, h[j], h[j + 1]));
-              if (tok0 + j < t.ntok) dst[static_cast<size_t>(j) * p.N] = static_cast<uint8_t>(two);
+              dst[static_cast<size_t>(j) * p.N] = static_cast<uint8_t>(two);
               if (tok0 + j + 1 < t.ntok) dst[static_cast<size_t>(j + 1) * p.N] = static_cast<uint8_t>(two >> 8);
             }
           };
