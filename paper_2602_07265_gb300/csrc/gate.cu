@@ -130,39 +130,41 @@ __device__ __forceinline__ void scan_group(const GateParams &p, const V *v, V *t
 }
 
 // The token's best groups (bit g) from the best two values of group lane >> shift, lowest<V>()
-// for experts that are not eligible.  *last, *rest: lanes of the last group taken and of
-// the best one left, -1 if there is none.
+// for experts that are not eligible.
 __device__ __forceinline__ uint32_t group_key(float worth) { return key_of(worth); }
 __device__ __forceinline__ Key64 group_key(Key64 worth) { return worth; }
 template <class V>
-__device__ __forceinline__ uint32_t best_groups(const GateParams &p, V top, V second, int shift, int *last, int *rest) {
+__device__ __forceinline__ uint32_t best_groups(const GateParams &p, V top, V second, int shift) {
   const int lane = threadIdx.x & 31;
   const V worth = worth_of(top, second, p.a.prm.group_top == 2 && second > lowest<V>());
   auto key = top > lowest<V>() ? group_key(worth) : decltype(group_key(worth))(0);
   uint32_t taken = 0;
-  *last = -1;
   for (int r = 0; r < p.a.prm.top_groups; ++r) {
     const auto best = warp_max(key);
     if (best == 0) break;
-    *last = __ffs(__ballot_sync(kAll, key == best)) - 1;
-    const int g = *last >> shift;
+    const int g = (__ffs(__ballot_sync(kAll, key == best)) - 1) >> shift;
     taken |= 1u << g;
     if (lane >> shift == g) key = 0;
   }
-  const auto left = warp_max(key);
-  *rest = left != 0 ? __ffs(__ballot_sync(kAll, key == left)) - 1 : -1;
   return taken;
 }
-// Of fp32 values: by how much the last group taken beats the best one left (the largest number if none
-// is left), and the largest magnitude among the values of these two that count.
-__device__ __forceinline__ void group_gap(const GateParams &p, float top, float second, int last, int rest, float *gap,
-                                          float *size) {
-  const bool both = p.a.prm.group_top == 2 && second > -INFINITY;
-  const float worth = worth_of(top, second, both), mine = fmaxf(fabsf(top), both ? fabsf(second) : 0.f);
-  const float w0 = __shfl_sync(kAll, worth, last & 31), w1 = __shfl_sync(kAll, worth, rest & 31);
-  const float m0 = __shfl_sync(kAll, mine, last & 31), m1 = __shfl_sync(kAll, mine, rest & 31);
-  *gap = rest >= 0 ? w0 - w1 : FLT_MAX;
-  *size = rest >= 0 ? fmaxf(m0, m1) : 0.f;
+// Whether fp32 leaves the choice of groups `taken` open: whether some group taken may be worth less
+// than some group left.  Each worth is off by what its own values' size gives, which a sum of two does not
+// show (s + 1000 and s' - 1000 add up to s + s'), and two groups' scores by `slack` against each
+// other.  A value rounds by 2^-24 of itself where the bias is added, a sum of two by 2^-24 of
+// at most twice the larger: 2^-23 of the value, 2^-22 of the larger one and, with as much again to spare, 2^-21.
+__device__ __forceinline__ bool groups_near(const GateParams &p, float top, float second, int shift, uint32_t taken,
+                                            float slack) {
+  const int lane = threadIdx.x & 31;
+  const bool any = top > -INFINITY, both = p.a.prm.group_top == 2 && second > -INFINITY;
+  const bool in = any && (taken >> (lane >> shift)) & 1u;
+  const float worth = worth_of(top, second, both);
+  const float size = fminf(fmaxf(fabsf(top), both ? fabsf(second) : 0.f), FLT_MAX);
+  const float off = size * (both ? 0x1p-21f : 0x1p-23f);
+  const uint32_t least = __reduce_min_sync(kAll, in ? key_of(__fsub_rd(worth, off)) : kAll);
+  const uint32_t most = __reduce_max_sync(kAll, any && !in ? key_of(__fadd_ru(worth, off)) : 0u);
+  // (Infinite worths on both sides leave NaN: near.)
+  return most != 0 && !(__fsub_rd(value_of(least), value_of(most)) >= (p.a.prm.group_top == 2 ? 2.f * slack : slack));
 }
 
 // Lane r gets the r-th best (r < rounds) of the values c, -1 where none above -infinity is left.
@@ -448,9 +450,8 @@ __device__ __noinline__ int exact_row(const GateParams &p, int t, float m, Two *
   uint32_t taken = kAll;
   if (p.a.prm.top_groups < p.a.prm.n_groups) {
     Key64 top, second;
-    int last, rest;
     scan_group(p, key, &top, &second);
-    taken = best_groups(p, top, second, p.scan_shift, &last, &rest);
+    taken = best_groups(p, top, second, p.scan_shift);
     __syncwarp();
   }
   // What decides between experts: without a bias the logits, as in the fp32 pass.  The winners are among
@@ -590,19 +591,19 @@ __global__ void __launch_bounds__(32 * kWarps, kE <= 8 ? 8 : kE <= 12 ? 6 : kE <
   // Groups and experts.
   const bool biased = a.bias != nullptr;
   const bool sums = a.prm.group_top == 2 && a.prm.top_groups < a.prm.n_groups;
-  float gap = FLT_MAX, size = 0.f;
+  bool groups = false;   // their choice is open
   uint32_t chosen = kAll;
 #pragma unroll
   for (int j = 0; j < kE; ++j) s[j] = biased || sums ? s[j] + bias[j] : l[j];
   if (a.prm.top_groups < a.prm.n_groups) {
     float top = -INFINITY, second = -INFINITY;
-    int last, rest;
+    uint32_t taken;
     if (p.group_shift >= 0) {
       // Groups of whole lanes: the lanes of a group exchange their best two.
 #pragma unroll
       for (int j = 0; j < kE; ++j) take(s[j], &top, &second);
       join_best(p.group_shift, &top, &second);
-      const uint32_t taken = best_groups(p, top, second, p.group_shift, &last, &rest);
+      taken = best_groups(p, top, second, p.group_shift);
       chosen = (taken >> (lane >> p.group_shift)) & 1u ? kAll : 0u;
     } else {
       float *values = reinterpret_cast<float *>(shared);
@@ -611,7 +612,7 @@ __global__ void __launch_bounds__(32 * kWarps, kE <= 8 ? 8 : kE <= 12 ? 6 : kE <
         if (lane * kE + j < N) values[lane * kE + j] = s[j];
       __syncwarp();
       scan_group(p, values, &top, &second);
-      const uint32_t taken = best_groups(p, top, second, p.scan_shift, &last, &rest);
+      taken = best_groups(p, top, second, p.scan_shift);
       chosen = 0;
 #pragma unroll
       for (int j = 0; j < kE; ++j) {
@@ -619,7 +620,8 @@ __global__ void __launch_bounds__(32 * kWarps, kE <= 8 ? 8 : kE <= 12 ? 6 : kE <
         if (g < 32 && (taken >> g) & 1u) chosen |= 1u << j;
       }
     }
-    group_gap(p, top, second, last, rest, &gap, &size);
+    if (biased || sums)
+      groups = groups_near(p, top, second, p.group_shift >= 0 ? p.group_shift : p.scan_shift, taken, slack);
 #pragma unroll
     for (int j = 0; j < kE; ++j) s[j] = (chosen >> j) & 1u ? (biased ? s[j] : l[j]) : -INFINITY;
   }
@@ -631,8 +633,7 @@ __global__ void __launch_bounds__(32 * kWarps, kE <= 8 ? 8 : kE <= 12 ? 6 : kE <
   // The winner's score and choice value, as above.
   const float lw = id >= 0 ? fminf(logit_at(p, t, id), FLT_MAX) : 0.f, bw = id >= 0 && biased ? a.bias[id] : 0.f;
   float score = id >= 0 ? score_of(softmax, lw, m, sum) : 0.f;
-  // Did a gap decide that fp32 does not resolve?  Adding the bias rounds too, by 2^-24 of
-  // the value; a group's sum by twice that more, so two groups are off by 2^-21 of the largest value.
+  // Did a gap decide that fp32 does not resolve?  Adding the bias rounds too, by 2^-24 of the value.
   if (biased || sums) {
     const float value = score + bw;
     float big = 0.f;
@@ -641,9 +642,6 @@ __global__ void __launch_bounds__(32 * kWarps, kE <= 8 ? 8 : kE <= 12 ? 6 : kE <
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, shfl_xor(big, o));
     }
-    // (The group's gap is the same in all lanes.)
-    // (Sums beyond fp32's range leave NaN.)
-    const bool groups = !(gap >= (sums ? 2.f * slack + 0x1p-20f * size : slack + 0x1p-22f * size));
     bool near = groups;
     const float limit = slack + 0x1p-22f * big;
     if (biased) {

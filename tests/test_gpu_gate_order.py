@@ -1,0 +1,52 @@
+"""xshare_gate's order of choice values against the plain 64-bit form, where fp32 misleads."""
+import numpy as np
+import pytest
+import torch
+
+import ops_reference as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def ops():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a CUDA GPU")
+    from paper_2602_07265_gb300 import _build
+    _build.build()
+    from paper_2602_07265_gb300 import ops
+    return ops
+
+
+def ids_of(ops, logits, k, scoring, bias=None, **kw):
+    B = logits.shape[0]
+    ids, w = torch.full((B, k), 77, dtype=torch.int32, device=DEV), torch.empty(B, k, device=DEV)
+    ops.xshare_gate(logits.to(DEV), k, ops.gate_params(scoring, **kw), ids, w, bias=None if bias is None else bias.to(DEV))
+    return ids.cpu().numpy()
+
+
+def check(ops, logits, k, scoring, bias=None, **kw):
+    want = R.gate(logits.numpy(), k, scoring, bias=None if bias is None else bias.numpy(), **kw)[0]
+    got = ids_of(ops, logits, k, scoring, bias, **kw)
+    assert np.array_equal(got, want), (int((got != want).any(1).sum()), "rows differ")
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("G,size,top", [(3, 2, 2), (8, 8, 3), (5, 7, 2), (32, 3, 9), (4, 64, 3)])
+def test_groups_whose_values_cancel(ops, scoring, G, size, top):
+    """One group holds a large positive and a large negative bias: fp32 knows its worth to 2^-14
+    or so, wherever among the groups it comes out, while the others' worths lie 2^-12 apart."""
+    g = torch.Generator().manual_seed(G)
+    B, N = 4000, G * size
+    bias = torch.zeros(G, size)
+    bias[:, 2:] = -0.9             # the first two experts make a group's worth
+    at = G // 2
+    # The group's third value must not come near: far below in the group with the large pair.
+    bias[at] = -3000.0
+    bias[at, 0], bias[at, 1] = 1000.0, -1000.0
+    l = torch.full((B, G, size), 0.5)
+    spread = 2e-4 if scoring == "sigmoid" else 2e-4 * N / 4
+    l[:, :, :2] += spread * torch.randn(B, G, 2, generator=g)
+    check(ops, l.reshape(B, N).contiguous(), min(top * size, 16) if size < 8 else 8, scoring, bias.reshape(N).contiguous(),
+          n_groups=G, top_groups=top, group_top=2)
