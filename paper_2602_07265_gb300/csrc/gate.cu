@@ -387,6 +387,27 @@ __device__ __forceinline__ uint32_t look_up_batch(const GateParams &p, int t, in
   return ok;
 }
 
+// Whether an expert of the groups `taken` comes within `limit` of the choice value v (logit l0, bias b0)
+// without being its equal.  For rows where the last winner and the next are equal: the ones behind
+// them may still be larger in truth.
+__device__ __noinline__ bool border_near(const GateParams &p, int t, float m, float sum, uint32_t taken, float v, float l0,
+                                         float b0, float limit) {
+  const int lane = threadIdx.x & 31;
+  const bool softmax = p.a.prm.scoring == XS_SCORE_SOFTMAX;
+  bool near = false;
+#pragma unroll 1
+  for (int e = lane; e - lane < p.a.N; e += 32 * kBatch) {
+    float l[kBatch], b[kBatch];
+    const uint32_t ok = look_up_batch(p, t, e, m, l, b);
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const bool in = (ok >> j) & 1u && (taken >> ((static_cast<uint32_t>(e + 32 * j) * p.magic) >> 21)) & 1u;
+      near |= in && fabsf(v - (score_of(softmax, l[j], m, sum) + b[j])) < limit && !(l[j] == l0 && b[j] == b0);
+    }
+  }
+  return __any_sync(kAll, near);
+}
+
 // 1 / the sum of a row's exponentials, m: the largest logit; sv: nullable, where they are left.
 __device__ __noinline__ Two row_scale(const GateParams &p, int t, float m, Two *sv) {
   const int lane = threadIdx.x & 31;
@@ -592,12 +613,11 @@ __global__ void __launch_bounds__(32 * kWarps, kE <= 8 ? 8 : kE <= 12 ? 6 : kE <
   const bool biased = a.bias != nullptr;
   const bool sums = a.prm.group_top == 2 && a.prm.top_groups < a.prm.n_groups;
   bool groups = false;   // their choice is open
-  uint32_t chosen = kAll;
+  uint32_t chosen = kAll, taken = kAll;
 #pragma unroll
   for (int j = 0; j < kE; ++j) s[j] = biased || sums ? s[j] + bias[j] : l[j];
   if (a.prm.top_groups < a.prm.n_groups) {
     float top = -INFINITY, second = -INFINITY;
-    uint32_t taken;
     if (p.group_shift >= 0) {
       // Groups of whole lanes: the lanes of a group exchange their best two.
 #pragma unroll
@@ -649,7 +669,11 @@ __global__ void __launch_bounds__(32 * kWarps, kE <= 8 ? 8 : kE <= 12 ? 6 : kE <
       const float v2 = __shfl_down_sync(kAll, value, 1);
       const float l2 = __shfl_down_sync(kAll, lw, 1), b2 = __shfl_down_sync(kAll, bw, 1);
       // The same logit and bias: a tie, which the lower index won.
-      near |= lane < k && id >= 0 && id2 >= 0 && value - v2 < limit && !(lw == l2 && bw == b2);
+      const bool same = lw == l2 && bw == b2;
+      near |= lane < k && id >= 0 && id2 >= 0 && value - v2 < limit && !same;
+      if (__any_sync(kAll, lane == k - 1 && id2 >= 0 && same))
+        near |= border_near(p, t, m, sum, taken, __shfl_sync(kAll, value, k - 1), __shfl_sync(kAll, lw, k - 1),
+                            __shfl_sync(kAll, bw, k - 1), limit);
     }
     if (__any_sync(kAll, near)) {
       // The candidates are enough if no other expert comes near the last winner (with fewer

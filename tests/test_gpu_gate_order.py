@@ -50,3 +50,30 @@ def test_groups_whose_values_cancel(ops, scoring, G, size, top):
     l[:, :, :2] += spread * torch.randn(B, G, 2, generator=g)
     check(ops, l.reshape(B, N).contiguous(), min(top * size, 16) if size < 8 else 8, scoring, bias.reshape(N).contiguous(),
           n_groups=G, top_groups=top, group_top=2)
+
+
+def logit(s):
+    return torch.log(s / (1 - s))
+
+
+@pytest.mark.parametrize("k,copies", [(1, 1), (1, 2), (3, 1), (3, 5), (8, 30)])
+@pytest.mark.parametrize("G", [1, 2])
+def test_equal_experts_before_one_that_is_near(ops, k, copies, G):
+    """The last winner has equals of a higher index, and behind them an expert whose real choice value is
+    larger or smaller by less than fp32 resolves: it wins or loses against all of them."""
+    g = torch.Generator().manual_seed(k + copies)
+    B, N, b0, b1 = 2000, 64, torch.tensor(0.1), torch.tensor(0.3)
+    base = torch.empty(B, dtype=torch.float32).uniform_(0.0, 2.0, generator=g)
+    l = torch.full((B, N), -5.0)
+    l[:, :k - 1] = 4 + torch.rand(B, k - 1, generator=g)     # winners before
+    l[:, k - 1:k + copies] = base[:, None]
+    s = torch.sigmoid(base.double()) + b0.double() - b1.double()
+    x = N // G - 1                                            # in the first group
+    l[:, x] = logit(s).float()
+    bias = torch.full((N,), 0.1)
+    bias[x] = 0.3
+    c = torch.sigmoid(l.double()) + bias.double()
+    gap = c[:, x] - c[:, k - 1]
+    keep = gap.abs() > 2.0 ** -36                             # what 40 bits tell for certain
+    assert keep.sum() > 1900 and 0.4 < (gap[keep] > 0).double().mean() < 0.6
+    check(ops, l[keep].contiguous(), k, "sigmoid", bias, n_groups=G, top_groups=1)
