@@ -72,7 +72,9 @@ size_t xshare_gate_workspace_size(int B, int N, int k);
  *   ids  = the k experts of largest c among the eligible ones of the top_groups
  *          best groups, best first; equal values: the lower index first, among
  *          groups too.  Values are ordered as real numbers: where fp32 cannot
- *          tell two of them apart, the row is evaluated again with about 40 bits.
+ *          tell two of them apart, the row is evaluated again with about 40 bits; where
+ *          those agree too, the larger bias goes first, then the larger logit, so that
+ *          equal biases (of zeros, say) leave experts in the order of their logits.
  *          (A choice value or a sum of two beyond fp32's range counts as infinite.)
  *   w    = s[ids], divided by their sum (renorm; 1 / (number routed) if the sum
  *          is 0), times scale.

@@ -215,6 +215,7 @@ __device__ __noinline__ int best_experts(const float (&c)[kE], int rounds) {
 struct Candidates {
   uint2 of[32];     // key, expert
   Key64 key[32];    // see rank_keys()
+  Key64 tie[32];
   int order[32];
 };
 
@@ -343,16 +344,27 @@ __device__ __forceinline__ bool look_up(const GateParams &p, int t, int e, float
   return v > -INFINITY && *b > -INFINITY && (p.a.expert_mask == nullptr || p.a.expert_mask[e] != 0);
 }
 
-// The order of the n candidates in `sh` by key, in lane i < n that of the i-th: lane r gets the r-th expert.
-__device__ __forceinline__ int rank_keys(Candidates *sh, int n, Key64 key) {
+// What decides between equal pairs of choice values with a bias: the larger bias, then the larger
+// logit.  A pair loses what lies below its last bit or below fp32's range, of a sigmoid near 0 (e^l), near 1
+// (1 - e^-l) or of a softmax; with the same bias the logits tell which lost more, and of
+// equal sums the one with the larger bias has the smaller score, which lost more upwards.  So a bias of
+// zeros leaves the order of no bias.  Infinite values are equal.
+__device__ __forceinline__ Key64 tie_of(const GateParams &p, int t, int e, Key64 key) {
+  if (p.a.bias == nullptr || static_cast<uint32_t>(key >> 32) == key_of(INFINITY)) return 0;
+  return static_cast<Key64>(key_of(p.a.bias[e])) << 32 | key_of(fminf(logit_at(p, t, e), FLT_MAX));
+}
+
+// The order of the n candidates in `sh` by key and tie, in lane i < n those of the i-th: lane r gets the r-th expert.
+__device__ __forceinline__ int rank_keys(Candidates *sh, int n, Key64 key, Key64 tie) {
   const int lane = threadIdx.x & 31, id = lane < n ? static_cast<int>(sh->of[lane].y) : 0;
   sh->key[lane] = key;
+  sh->tie[lane] = tie;
   __syncwarp();
   int rank = 0;
 #pragma unroll 1
   for (int r = 0; r < n; ++r) {
-    const Key64 o = sh->key[r];
-    rank += o > key || (o == key && static_cast<int>(sh->of[r].y) < id);
+    const Key64 o = sh->key[r], u = sh->tie[r];
+    rank += o > key || (o == key && (u > tie || (u == tie && static_cast<int>(sh->of[r].y) < id)));
   }
   if (lane < n) sh->order[rank] = id;
   __syncwarp();
@@ -439,7 +451,8 @@ __device__ __noinline__ int near_row(const GateParams &p, int t, float m, int n,
   const int id = lane < n ? static_cast<int>(sh->of[lane].y) : 0;
   const float l = lane < n ? fminf(logit_at(p, t, id), FLT_MAX) : m;
   const Two s = softmax ? two_exp_diff(l, m) * row_scale(p, t, m, nullptr) : two_sigmoid(l);
-  return rank_keys(sh, n, key_of(add_any(s, Two{p.a.bias[id], 0.f})));
+  const Key64 key = key_of(add_any(s, Two{p.a.bias[id], 0.f}));
+  return rank_keys(sh, n, key, tie_of(p, t, id, key));
 }
 
 // The choice of row t again in pairs, sv[e] in shared memory; lane r gets the r-th expert.  m:
@@ -517,23 +530,29 @@ __device__ __noinline__ int exact_row(const GateParams &p, int t, float m, Two *
   }
   __syncwarp();
   if (n <= 32) {
-    const int id = rank_keys(sh, n, lane < n ? key[sh->of[lane].y] : 0);
+    const int mine = lane < n ? static_cast<int>(sh->of[lane].y) : 0;
+    const int id = rank_keys(sh, n, lane < n ? key[mine] : 0, tie_of(p, t, mine, key[mine]));
     return lane < k ? id : -1;
   }
-  // Many equal upper halves: k rounds over all keys.
+  // Many equal upper halves: k rounds over all keys, then over those that are equal to the largest.
   int id = -1;
 #pragma unroll 1
   for (int r = 0; r < k; ++r) {
-    Key64 mine = lowest<Key64>();
+    Key64 mine = lowest<Key64>(), tie = 0;
     int em = N;
-    for (int e = lane; e < N; e += 32)
-      if (key[e] > mine) {
-        mine = key[e];
-        em = e;
-      }
+    for (int e = lane; e < N; e += 32) mine = key[e] > mine ? key[e] : mine;
     const Key64 best = warp_max(mine);
     if (best == lowest<Key64>()) break;
-    const int win = __reduce_min_sync(kAll, static_cast<unsigned>(mine == best ? em : N));
+    for (int e = lane; e < N; e += 32)
+      if (key[e] == best) {
+        const Key64 u = tie_of(p, t, e, best);
+        if (em == N || u > tie) {
+          tie = u;
+          em = e;
+        }
+      }
+    const Key64 first = warp_max(tie);
+    const int win = __reduce_min_sync(kAll, static_cast<unsigned>(tie == first ? em : N));
     if (lane == r) id = win;
     if ((win & 31) == lane) key[win] = lowest<Key64>();
   }

@@ -72,7 +72,8 @@ XS_HD float power_of_two(int k) {
 #endif
 }
 
-// e^x for x <= 0, relative error below 2^-40 for x >= -80; 0 below -100.
+// e^x for x <= 0, within 2^-40 of its value and 2^-148 (the parts may be subnormal: the latter is the larger
+// from x = -75 down); 0 below -100.
 XS_HD Two two_exp(float x) {
   const bool none = !(x > -100.f);
   x = none ? 0.f : x;
@@ -102,7 +103,7 @@ XS_HD Two two_exp(float x) {
   return Two{s.hi * p0 * p1, s.lo * p0 * p1};
 }
 
-// 1 / (1 + e^-x), relative error below 2^-38 for |x| <= 80.
+// 1 / (1 + e^-x), within 2^-38 of its value and 2^-147; 0 for x below -100.
 XS_HD Two two_sigmoid(float x) {
   const Two e = two_exp(-fabsf(x)), one = Two{1.f, 0.f};
   return (x >= 0.f ? one : e) / (e + 1.f);

@@ -77,3 +77,26 @@ def test_equal_experts_before_one_that_is_near(ops, k, copies, G):
     keep = gap.abs() > 2.0 ** -36                             # what 40 bits tell for certain
     assert keep.sum() > 1900 and 0.4 < (gap[keep] > 0).double().mean() < 0.6
     check(ops, l[keep].contiguous(), k, "sigmoid", bias, n_groups=G, top_groups=1)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+def test_scores_below_the_range_of_fp32(ops, scoring):
+    """e^-100 and less: the choice values differ by orders of magnitude, and a bias of zeros changes nothing."""
+    for rows, k in (([[-130.0, -120, -110], [-105, -101, -104], [0, -120, -110], [-99, -100.5, -101.5], [-90, -95, -89]], 3),
+                    ([[-87.5, -88.0, -103.9, -150, -149, -600, -599, -400]], 5)):
+        l = torch.tensor(rows)
+        for n in range(1, k + 1):
+            check(ops, l, n, scoring, torch.zeros(l.shape[1]))
+            check(ops, l, n, scoring)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("N,k", [(20, 6), (64, 16), (256, 8), (1000, 16)])
+@pytest.mark.parametrize("lo,hi", [(-300, -90), (-200, 5), (30, 250), (-1e30, -1e29), (-20, 20), (-1e-20, 1e-20)])
+def test_a_bias_of_zeros_changes_nothing(ops, scoring, N, k, lo, hi):
+    """Scores that underflow, saturate or agree in all the bits that are looked at: equal biases leave the order to the
+    logits, for few such experts and for more than are kept as candidates."""
+    g = torch.Generator().manual_seed(N)
+    l = torch.empty(60, N).uniform_(lo, hi, generator=g)
+    want = R.gate(l.numpy(), k, scoring)[0]
+    assert np.array_equal(ids_of(ops, l, k, scoring, torch.zeros(N)), want)

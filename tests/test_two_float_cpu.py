@@ -77,3 +77,21 @@ def test_sums_are_normalised(lib):
     got = run(lib.run_add, x, b)
     want = np.array([float(1 / (1 + (-Decimal(float(v))).exp()) + Decimal(float(u))) for v, u in zip(x, b)])
     assert np.all(np.abs(got - want) <= 2.0 ** -38 + 2.0 ** -46 * np.abs(want))
+
+
+def test_small_values(lib):
+    """Down to the smallest numbers, whose last bit is 2^-149 whatever the value."""
+    getcontext().prec = 60
+    x = points(-100.0, 0.0)
+    want = np.array([float(Decimal(float(v)).exp()) for v in x])
+    assert np.all(np.abs(run(lib.run_exp, x) - want) <= 2.0 ** -40 * want + 2.0 ** -148)
+    want = np.array([float(1 / (1 + (-Decimal(float(v))).exp())) for v in x])
+    assert np.all(np.abs(run(lib.run_sigmoid, x) - want) <= 2.0 ** -38 * want + 2.0 ** -147)
+    assert np.all(np.abs(run(lib.run_sigmoid, -x) - 1 + want) <= 2.0 ** -38)
+
+
+def test_the_order_is_kept(lib):
+    """Larger arguments never give smaller values, into the subnormal numbers."""
+    x = np.sort(points(-110.0, 0.0))
+    for fn in (lib.run_exp, lib.run_sigmoid):
+        assert np.all(np.diff(run(fn, x)) >= 0)
