@@ -129,18 +129,14 @@ __device__ __forceinline__ void scan_group(const GateParams &p, const V *v, V *t
   join_best(shift, top, second);
 }
 
-// The token's best groups (bit g) from the best two values of group lane >> shift, lowest<V>()
+// The token's best groups (bit g) from the best two values of group lane >> shift, -infinity
 // for experts that are not eligible.
-__device__ __forceinline__ uint32_t group_key(float worth) { return key_of(worth); }
-__device__ __forceinline__ Key64 group_key(Key64 worth) { return worth; }
-template <class V>
-__device__ __forceinline__ uint32_t best_groups(const GateParams &p, V top, V second, int shift) {
+__device__ __forceinline__ uint32_t best_groups(const GateParams &p, float top, float second, int shift) {
   const int lane = threadIdx.x & 31;
-  const V worth = worth_of(top, second, p.a.prm.group_top == 2 && second > lowest<V>());
-  auto key = top > lowest<V>() ? group_key(worth) : decltype(group_key(worth))(0);
-  uint32_t taken = 0;
+  const float worth = worth_of(top, second, p.a.prm.group_top == 2 && second > -INFINITY);
+  uint32_t key = top > -INFINITY ? key_of(worth) : 0u, taken = 0;
   for (int r = 0; r < p.a.prm.top_groups; ++r) {
-    const auto best = warp_max(key);
+    const uint32_t best = warp_max(key);
     if (best == 0) break;
     const int g = (__ffs(__ballot_sync(kAll, key == best)) - 1) >> shift;
     taken |= 1u << g;
@@ -455,6 +451,77 @@ __device__ __noinline__ int near_row(const GateParams &p, int t, float m, int n,
   return rank_keys(sh, n, key, tie_of(p, t, id, key));
 }
 
+// The logits of the best two experts of group lane >> scan_shift by their choice values' pairs, key[e], and where
+// these are equal by bias and logit; -infinity where there is none.
+__device__ __noinline__ void best_logits(const GateParams &p, int t, const Key64 *key, float *l1, float *l2) {
+  const int lane = threadIdx.x & 31, shift = p.scan_shift, g = lane >> shift, sub = lane & ((1 << shift) - 1);
+  const Key64 none = key_of(-INFINITY);
+  Key64 k1 = lowest<Key64>(), k2 = k1, u1 = none, u2 = none;   // lower halves of u: the logits
+  auto take_both = [&](Key64 k, Key64 u) {
+    if (k > k1 || (k == k1 && u > u1)) {
+      k2 = k1;
+      u2 = u1;
+      k1 = k;
+      u1 = u;
+    } else if (k > k2 || (k == k2 && u > u2)) {
+      k2 = k;
+      u2 = u;
+    }
+  };
+  if (g < p.a.prm.n_groups)
+#pragma unroll 1
+    for (int e = g * p.gs + sub; e < (g + 1) * p.gs; e += 1 << shift)
+      if (key[e] > lowest<Key64>())
+        take_both(key[e], static_cast<Key64>(key_of(p.a.bias != nullptr ? p.a.bias[e] : 0.f)) << 32 |
+                              key_of(fminf(logit_at(p, t, e), FLT_MAX)));
+  for (int o = 1; o < 1 << shift; o <<= 1) {
+    const Key64 ka = shfl_xor(k1, o), ua = shfl_xor(u1, o), kb = shfl_xor(k2, o), ub = shfl_xor(u2, o);
+    take_both(ka, ua);
+    take_both(kb, ub);
+  }
+  *l1 = value_of(static_cast<uint32_t>(u1));
+  *l2 = value_of(static_cast<uint32_t>(u2));
+}
+
+// The best groups by their worths in pairs.  Scores below e^-75 lose bits of a pair and then
+// all of them, so groups worth less than 2^-100, whose biases are 0 or cancel, are compared by the
+// sum of e^(l - m), m: the largest logit among those still left.
+__device__ __noinline__ uint32_t exact_groups(const GateParams &p, int t, const Key64 *key) {
+  const int lane = threadIdx.x & 31, shift = p.scan_shift;
+  Key64 top, second;
+  scan_group(p, key, &top, &second);
+  const bool both = p.a.prm.group_top == 2 && second > lowest<Key64>();
+  const Key64 zero = key_of(Two{0.f, 0.f});
+  Key64 worth = top > lowest<Key64>() ? worth_of(top, second, both) : 0;
+  const bool tiny = worth >= zero && two_of(worth).hi < 0x1p-100f;
+  float l1 = -INFINITY, l2 = -INFINITY;
+  if (__any_sync(kAll, tiny)) {
+    best_logits(p, t, key, &l1, &l2);
+    if (tiny) worth = zero;
+  }
+  uint32_t taken = 0;
+  for (int r = 0; r < p.a.prm.top_groups; ++r) {
+    const Key64 best = warp_max(worth);
+    if (best == 0) break;
+    bool first = worth == best;
+    if (best == zero) {
+      const float m = value_of(__reduce_max_sync(kAll, first ? key_of(l1) : 0u));
+      Key64 part = 0;
+      if (first) {
+        Two sum = two_exp_diff(l1, m);
+        if (both) sum = sum + two_exp_diff(l2, m);
+        part = key_of(sum);
+      }
+      const Key64 most = warp_max(part);
+      first = first && part == most;
+    }
+    const int g = (__ffs(__ballot_sync(kAll, first)) - 1) >> shift;
+    taken |= 1u << g;
+    if (lane >> shift == g) worth = 0;
+  }
+  return taken;
+}
+
 // The choice of row t again in pairs, sv[e] in shared memory; lane r gets the r-th expert.  m:
 // the largest logit.
 __device__ __noinline__ int exact_row(const GateParams &p, int t, float m, Two *sv, Candidates *sh) {
@@ -483,9 +550,7 @@ __device__ __noinline__ int exact_row(const GateParams &p, int t, float m, Two *
   __syncwarp();
   uint32_t taken = kAll;
   if (p.a.prm.top_groups < p.a.prm.n_groups) {
-    Key64 top, second;
-    scan_group(p, key, &top, &second);
-    taken = best_groups(p, top, second, p.scan_shift);
+    taken = exact_groups(p, t, key);
     __syncwarp();
   }
   // What decides between experts: without a bias the logits, as in the fp32 pass.  The winners are among

@@ -100,3 +100,22 @@ def test_a_bias_of_zeros_changes_nothing(ops, scoring, N, k, lo, hi):
     l = torch.empty(60, N).uniform_(lo, hi, generator=g)
     want = R.gate(l.numpy(), k, scoring)[0]
     assert np.array_equal(ids_of(ops, l, k, scoring, torch.zeros(N)), want)
+
+
+@pytest.mark.parametrize("scoring", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("G,size,top", [(4, 2, 2), (8, 8, 3), (5, 7, 2), (32, 3, 9), (4, 64, 3), (8, 1, 5)])
+@pytest.mark.parametrize("group_top", [1, 2])
+@pytest.mark.parametrize("lo,hi", [(-140, -110), (-115, -80), (-400, -70), (-90, -60), (-300, 0)])
+def test_groups_of_scores_below_the_range_of_fp32(ops, scoring, G, size, top, group_top, lo, hi):
+    """Groups whose worth underflows keep the order of the real sums, without a bias and with one of zeros
+    (a softmax has them below its largest score)."""
+    g = torch.Generator().manual_seed(G + size)
+    l = torch.empty(100, G * size).uniform_(lo, hi, generator=g)
+    if scoring == "softmax":
+        l[:, 0] = 2.0
+    k = min(top * size, 8)
+    kw = dict(n_groups=G, top_groups=top, group_top=group_top)
+    check(ops, l, k, scoring, **kw)
+    # The reference takes groups by logits where there is no bias, which is the order of the scores too.
+    want = R.gate(l.numpy(), k, scoring, **kw)[0]
+    assert np.array_equal(ids_of(ops, l, k, scoring, torch.zeros(G * size), **kw), want)
