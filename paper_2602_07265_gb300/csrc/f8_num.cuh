@@ -15,23 +15,24 @@ __device__ __forceinline__ float f8_scale(float amax) { return __fdiv_rn(fmaxf(a
 // with r the rounded reciprocal, one step of q += r (x - q s) makes q = x r faithful,
 // a second one correct (both residuals are exact fused operations).  Five multiply-adds for
 // two values (packed pairs) instead of a division each; scales near the ends of the
-// exponent range, where a residual could underflow, take the division.
+// exponent range, where a residual could underflow, take the division.  All of it with -x and -r: the
+// residual of a zero is +0, and -0 + r 0 would be +0, where -0 - r 0 stays -0.
 struct F8Divider {
   float s0, s1;        // of the first and the second of two values
-  uint64_t r2, ns2;
+  uint64_t nr2, s2;
   bool plain;
   // r0, r1: 1 / s0, 1 / s1, rounded.
   __device__ __forceinline__ F8Divider(float a, float b, float r0, float r1)
-      : s0(a), s1(b), r2(ptx::pack2(r0, r1)), ns2(ptx::pack2(-a, -b)),
+      : s0(a), s1(b), nr2(ptx::pack2(-r0, -r1)), s2(ptx::pack2(a, b)),
         plain(!(fminf(a, b) > 0x1p-60f && fmaxf(a, b) < 0x1p60f)) {}
   __device__ __forceinline__ F8Divider(float s, float r) : F8Divider(s, s, r, r) {}
   __device__ __forceinline__ explicit F8Divider(float s) : F8Divider(s, 1.f / s) {}
   // Two quotients; not for `plain`.
   __device__ __forceinline__ float2 operator()(float a, float b) const {
-    const uint64_t x = ptx::pack2(a, b);
-    uint64_t q = ptx::mul2(x, r2);
-    q = ptx::fma2(ptx::fma2(q, ns2, x), r2, q);
-    return ptx::unpack2(ptx::fma2(ptx::fma2(q, ns2, x), r2, q));
+    const uint64_t nx = ptx::pack2(-a, -b);
+    uint64_t q = ptx::mul2(nx, nr2);
+    q = ptx::fma2(ptx::fma2(q, s2, nx), nr2, q);
+    return ptx::unpack2(ptx::fma2(ptx::fma2(q, s2, nx), nr2, q));
   }
   __device__ __forceinline__ float2 slow(float a, float b) const {
     return make_float2(__fdiv_rn(a, s0), __fdiv_rn(b, s1));

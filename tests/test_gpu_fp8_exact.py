@@ -63,3 +63,32 @@ def test_activations_on_the_border_of_two_values(ops, B):
         ops.xshare_experts_fp8(xs, ids, w, ex, y, ws)
         want = torch.from_numpy(hq[0, n0:n0 + d] * float(hs[0, n0 // 128])).to(torch.bfloat16).to(DEV)
         assert torch.equal(y, want.expand(B, d))
+
+
+def bytes_of(x, rows):
+    """The quantised bytes by their definition: the quotient rounded to 32 bits, then to e4m3."""
+    s = R.quant(x, rows)[1]
+    big = np.repeat(np.repeat(s, rows, 0)[:x.shape[0]], 128, 1)[:, :x.shape[1]]
+    q = (x.astype(np.float64) / big.astype(np.float64)).astype(np.float32)
+    return torch.from_numpy(q).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("K", [128, 130, 133, 132, 144, 1000])   # every width of access
+@pytest.mark.parametrize("amax", [3.0, 1e-30, 1e30])              # both ways to divide
+def test_signs_of_zeros(ops, dtype, K, amax):
+    """-0, and values so small that they round to a zero, keep their sign, whatever the scale."""
+    if dtype is torch.float16 and amax != 3.0:
+        pytest.skip("beyond fp16")
+    g = torch.Generator().manual_seed(K)
+    x = torch.randn(200, K, generator=g) * amax
+    x[torch.rand(200, K, generator=g) < 0.3] = 0.0
+    x[torch.rand(200, K, generator=g) < 0.2] *= 1e-6
+    x = torch.where(torch.rand(200, K, generator=g) < 0.5, -x, x).to(dtype)
+    assert ((x == 0) & torch.signbit(x)).any()
+    d = x.to(DEV)
+    for rows, call in ((1, ops.xshare_quant_fp8_rows), (128, ops.xshare_quant_fp8_blocks)):
+        q = torch.empty(200, K, dtype=ops.FP8, device=DEV)
+        s = torch.empty(-(-200 // rows), -(-K // 128), device=DEV)
+        call(d, q, s)
+        assert np.array_equal(q.view(torch.uint8).cpu().numpy(), bytes_of(x.float().numpy(), rows))
