@@ -122,8 +122,13 @@ def xshare_gate(logits: torch.Tensor, k: int, params: GateParams, topk_ids: torc
                 token_mask: Optional[torch.Tensor] = None, scores_out: Optional[torch.Tensor] = None,
                 expert_counts: Optional[torch.Tensor] = None, expert_offsets: Optional[torch.Tensor] = None,
                 perm: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> None:
-    """Routes tokens by their router logits [B, N]; see xshare_ops.h."""
+    """Routes tokens by their router logits [B, N] into topk_ids and topk_w [B, k] and scores_out
+    [B, N]; see xshare_ops.h.  The buffers of one dimension may be longer than is needed."""
     B, N = logits.shape
+    _shaped(topk_ids, "topk_ids", B, k)
+    _shaped(topk_w, "topk_w", B, k)
+    if scores_out is not None:
+        _shaped(scores_out, "scores_out", B, N)
     dev = _current_device(logits)
     ws = ws_bytes = bias_p = emask_p = tmask_p = scores_p = counts_p = offsets_p = perm_p = None
     if workspace is not None:

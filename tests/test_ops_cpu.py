@@ -163,3 +163,19 @@ def test_reference_rounding_is_torchs():
                         np.nextafter(mid.astype(np.float32), np.float32(500))]).astype(np.float32)
     x = np.concatenate([x, -x])
     assert np.array_equal(R.e4m3_round(x), torch.from_numpy(x).to(torch.float8_e4m3fn).double().numpy())
+
+
+def gate_tensors(B=4, N=8, k=2):
+    return dict(logits=torch.zeros(B, N), k=k, topk_ids=torch.zeros(B, k, dtype=torch.int32), topk_w=torch.zeros(B, k),
+                scores_out=torch.zeros(B, N))
+
+
+@pytest.mark.parametrize("name,shape", [("topk_ids", (2, 4)), ("topk_ids", (4, 6)), ("topk_ids", (8,)), ("topk_ids", (3, 2)),
+                                        ("topk_w", (2, 4)), ("topk_w", (4, 3)), ("topk_w", (5, 2)),
+                                        ("scores_out", (8, 4)), ("scores_out", (4, 9)), ("scores_out", (32,))])
+def test_gate_binding_refuses_shapes(ops, name, shape):
+    """Buffers that are large enough but of another shape: their rows would not be the tokens'."""
+    a = gate_tensors()
+    a[name] = torch.zeros(*shape, dtype=a[name].dtype)
+    with pytest.raises(ValueError, match=name):
+        ops.xshare_gate(a.pop("logits"), a.pop("k"), ops.gate_params(), a.pop("topk_ids"), a.pop("topk_w"), **a)
