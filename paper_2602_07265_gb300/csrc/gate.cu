@@ -367,13 +367,6 @@ __device__ __forceinline__ int rank_keys(Candidates *sh, int n, Key64 key, Key64
   return lane < n ? sh->order[lane] : -1;
 }
 
-// e^(l - m) as a pair, for l and m of any size with l <= m.
-__device__ __forceinline__ Two two_exp_diff(float l, float m) {
-  // The exponential of the difference's upper part times 1 + the lower.
-  const Two d = two_sum(l, -m);
-  return two_exp(fminf(d.hi, 0.f)) * quick_two(1.f, d.hi > -100.f ? d.lo : 0.f);
-}
-
 // The second look takes kBatch experts of a lane at a time, e, e + 32, ..., looked up before any
 // arithmetic: a pair's exponential is a chain of 200 operations, so several run side by side.
 constexpr int kBatch = 4;

@@ -95,3 +95,28 @@ def test_the_order_is_kept(lib):
     x = np.sort(points(-110.0, 0.0))
     for fn in (lib.run_exp, lib.run_sigmoid):
         assert np.all(np.diff(run(fn, x)) >= 0)
+
+
+DIFF = r"""
+#include "two_float.cuh"
+extern "C" void run_exp_diff(const float *l, const float *m, double *y, int n) {
+  for (int i = 0; i < n; ++i) { xs::Two t = xs::two_exp_diff(l[i], m[i]); y[i] = (double)t.hi + t.lo; }
+}
+"""
+
+
+def test_exp_of_a_difference(tmp_path):
+    """Logits whose difference fp32 does not hold, far apart: the rounding of l - m is made good."""
+    getcontext().prec = 60
+    src, out = tmp_path / "diff.cpp", tmp_path / "diff.so"
+    src.write_text(DIFF)
+    subprocess.run(["g++", "-O2", "-std=c++17", "-ffp-contract=off", "-shared", "-fPIC", "-I", CSRC, "-x", "c++", str(src),
+                    "-o", str(out)], check=True, capture_output=True, text=True)
+    lib = ctypes.CDLL(str(out))
+    rng = np.random.default_rng(3)
+    m = rng.uniform(-3, 40, 4000).astype(np.float32)
+    l = (m.astype(np.float64) - rng.uniform(0, 75, 4000)).astype(np.float32)
+    l = np.minimum(l, m)
+    got = run(lib.run_exp_diff, l, m)
+    want = np.array([float((Decimal(float(a)) - Decimal(float(b))).exp()) for a, b in zip(l, m)])
+    assert np.all(np.abs(got - want) <= 1.5 * 2.0 ** -40 * want + 2.0 ** -148), (np.abs(got - want) / want).max()
