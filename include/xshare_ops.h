@@ -124,7 +124,8 @@ size_t xshare_matmul_fp8_workspace_size(int M, int N, int K, int E);
  *   offsets: NULL (then E == 1 and every row takes matrix 0), or [E + 1] int32,
  *          device: rows offsets[e] .. offsets[e + 1] - 1 take matrix e.  Entries
  *          are clamped to 0 .. M and made non-decreasing; rows before the first
- *          and behind the last entry are neither read nor written.
+ *          and behind the last entry are not written and have no influence (tiles that
+ *          end or begin beside them are loaded whole, so a of all M rows is read).
  *   y [M, N] of type y_dtype (XS_*).
  *   stats: nullable; status is set (XS_DEV_*), and with offsets n_pairs = rows
  *          and n_used = matrices with a row; the other fields are 0.

@@ -88,7 +88,7 @@ struct F8Params {
   int rows, N, KB, NB;     // NB: scale rows of a matrix, ceil(N / 128)
   int edge;                // box rows of a matrix's last 128-row block, if that is not whole
   int early;
-  uint32_t hold;           // see F8Args
+  uint32_t hold;
   uint64_t wait_ns;
 };
 
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
   const uint32_t rank = cluster_ctarank();
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(full_bar(s), 1);
+      mbar_init(full_bar(s), 1 + (blockIdx.x == 0 && p.hold == s + 1u));   // hold: see F8Args
       mbar_init(empty_bar(s), 2);   // both issuers' MMAs
     }
     for (int b = 0; b < 4; ++b) {
@@ -394,7 +394,6 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
   if (warp < 4) regs_dec<kIssueRegs>();
   if (warp == 0) {
     // ------------------------------------------------ TMA producer
-    const uint32_t hold = blockIdx.x == 0 ? p.hold : 0;
     int stage = 0, kb = 0;
     uint32_t phase = 0;
     bool ok = true;
@@ -412,7 +411,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_kernel(const __grid_constant__
           if (rank == 0) mbar_arrive_expect_tx(full_bar(stage), step_bytes(t));
           load_b(t, kb, stage);
         }
-        if (i + 1 != hold) load_a(t, kb, stage);
+        load_a(t, kb, stage);
       }
       __syncwarp();
       if (++kb == KB && i + 1 < n_blocks) {

@@ -88,7 +88,7 @@ struct FewParams {
   int rows, N, KB, NB;     // NB: scale rows of a matrix, ceil(N / 128)
   int edge;                // box rows of a matrix's last 128-row block, if that is not whole
   int early;
-  uint32_t hold;           // see F8Args
+  uint32_t hold;
   uint64_t wait_ns;
 };
 
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
   const uint32_t rank = kSplit ? cluster_ctarank() : 0, ranks = kSplit ? cluster_nctarank() : 1;
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(full_bar(s), 1);
+      mbar_init(full_bar(s), 1 + (blockIdx.x == 0 && p.hold == s + 1u));   // hold: see F8Args
       mbar_init(empty_bar(s), 1);
     }
     for (int b = 0; b < kBufs; ++b) {
@@ -288,7 +288,6 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
   if (warp < 4) regs_dec<kIssueRegs>();
   if (warp == 0) {
     // ------------------------------------------------ TMA producer
-    const uint32_t hold = blockIdx.x == 0 ? p.hold : 0;
     int stage = 0, kb = kb_first, u = u_first;
     uint32_t phase = 0;
     bool ok = true;
@@ -305,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
           mbar_arrive_expect_tx(full_bar(stage), step_bytes(t));
           load_w(t, kb, stage);
         }
-        if (i + 1 != hold) load_x(t, kb, stage);
+        load_x(t, kb, stage);
       }
       __syncwarp();
       if (++kb == kb_end && i + 1 < n_blocks) {

@@ -114,7 +114,7 @@ struct F8Args {
   float *part;                 // few rows: f8_part_bytes(), partial sums of cut units
   int32_t *cnt;                // and [kF8Ctas] arrivals, zero at the start
   uint64_t wait_ns;            // limit of the MMA issuers' waits for operands (the others': kF8WaitNs)
-  uint32_t hold;               // self-test: CTA 0 never loads the tokens of its K block hold - 1; 0: loads all
+  uint32_t hold;               // self-test: in CTA 0 the barrier of stage hold - 1 waits for an arrival that never comes; 0: none
 };
 // The product kernels are launched with 168 registers for each of their 384 threads and hand
 // them out again by warpgroup.  A split that asks for more than the launch holds would wait for

@@ -8,8 +8,8 @@
 // all of them must be told so.  No fault, trap or unbounded loop is involved.
 //
 // The waits of the float8 products are made to run out in the products themselves:
-// one CTA leaves out one load, with a short limit, so that the kernels' own way
-// out is what runs.
+// one CTA has a barrier that waits for one arrival too many, with a short limit, so
+// that the kernels' own way out is what runs.
 #include <cuda_runtime.h>
 
 #include "ops_internal.cuh"
@@ -60,7 +60,7 @@ __global__ void wait_timeout_kernel(xs_stats *stats, unsigned long long budget_n
 // Set by this host thread for a product that it launches later.
 struct Hold {
   int launches = -1;   // products before it; -1: none
-  uint32_t block = 0;
+  uint32_t stage = 0;
   uint64_t wait_ns = 0;
 };
 thread_local Hold t_hold;
@@ -71,18 +71,18 @@ void f8_waits(F8Args *a) {
   a->wait_ns = kF8WaitNs;
   if (t_hold.launches < 0 || t_hold.launches-- > 0) return;
   a->wait_ns = t_hold.wait_ns;
-  a->hold = t_hold.block + 1;
+  a->hold = t_hold.stage + 1;
 }
 
 }  // namespace xs
 
 // For tests: of the float8 products that this host thread launches from now on, the one after
-// `launches` others waits at most wait_ns at a time, and its CTA 0 leaves out the tokens
-// of its K block `block` (ends without the timeout if it has none).
-extern "C" int xshare_selftest_f8_hold(int launches, uint32_t block, uint64_t wait_ns) {
-  if (launches < 0 || block > 1u << 30 || wait_ns == 0 || wait_ns > xs::kF8WaitNs) return XS_ERR_PARAM;
+// `launches` others waits for operands for wait_ns at most, and the K block `stage` of its CTA 0, one of
+// the first that its ring holds, never counts as loaded.
+extern "C" int xshare_selftest_f8_hold(int launches, uint32_t stage, uint64_t wait_ns) {
+  if (launches < 0 || stage > 1u << 30 || wait_ns == 0 || wait_ns > xs::kF8WaitNs) return XS_ERR_PARAM;
   xs::t_hold.launches = launches;
-  xs::t_hold.block = block;
+  xs::t_hold.stage = stage;
   xs::t_hold.wait_ns = wait_ns;
   return XS_OK;
 }

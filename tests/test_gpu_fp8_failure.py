@@ -1,7 +1,7 @@
 """Waits that run out inside the float8 products, without a GPU fault.
 
-One CTA leaves out one load, so that its barrier stays open; after a limit of 20 ms the
-kernel gives up by its own way out.  The call has to report it, and the next call on
+One CTA has a barrier that waits for one arrival too many; after a limit of 20 ms the kernel
+gives up by its own way out.  The call has to report it, and the next call on
 the same workspace has to be right.
 """
 import ctypes
@@ -49,10 +49,11 @@ def blocks_of(ops, w):
     return q, s
 
 
-# Rows, columns, K, matrices, and the K block of CTA 0 that never becomes full.
+# Rows, columns, K, matrices, and the K block of CTA 0 that never becomes full (one of the first
+# that the ring holds: four with tiles of 64, else five or six).
 PRODUCTS = [(3, 1000, 2048, 1, 0), (20, 512, 2048, 1, 1),          # a cluster for every unit
-            (1, 32768, 7168, 1, 3), (8, 32768, 7168, 1, 40),       # units cut between CTAs
-            (320, 4096, 512, 8, 0), (320, 4096, 640, 8, 4),        # whole units, tiles of 64
+            (1, 32768, 7168, 1, 3), (8, 32768, 7168, 1, 4),       # units cut between CTAs
+            (320, 4096, 512, 8, 0), (320, 4096, 640, 8, 3),        # whole units, tiles of 64
             (190, 9000, 256, 8, 1),                                # and of 32
             (600, 1000, 640, 1, 2), (300, 4096, 384, 1, 0), (1500, 1040, 512, 3, 3)]   # CTA pairs
 
