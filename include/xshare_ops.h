@@ -148,8 +148,8 @@ size_t xshare_experts_fp8_workspace_size(int B, int N, int k, int d, int F);
 
 /* The experts of a routed batch on float8 weights:
  *   q(x_t): x_t in 1 x 128 blocks;   g, u = W_gate[e] q(x_t), W_up[e] q(x_t)  (fp32)
- *   h = silu(g) * u in fp32 (silu within 2^-20 + |g| 2^-24 of its value; e^-g beyond fp32's
- *   range counts as infinite), q(h) in 1 x 128 blocks;   o_ts = W_down[e] q(h)  (fp32
+ *   h = silu(g) * u in fp32 (silu within 2^-20 + |g| 2^-24 of its value; 0 where e^-g
+ *   passes 2^126), q(h) in 1 x 128 blocks;   o_ts = W_down[e] q(h)  (fp32
  *   sums; above 64 slots per expert kept in fp16 with one power of two per 64 columns)
  *   y_t = sum over slots s, in order, of topk_w[t, s] o_ts, fp32, rounded once to bf16.
  *
