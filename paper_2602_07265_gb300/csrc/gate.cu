@@ -14,7 +14,7 @@
 // fp32 scores carry an error, and two choice values nearer than that would come
 // out in an order that depends on the rounding of expf.  Where there is a bias (or
 // a group is worth a sum) the kernel looks at the gaps that decided: between
-// successive winners, the last winner and the next, the last group and the next.
+// successive winners, the last winner and the next, any group taken and any left.
 // A row with a gap below the error bound is evaluated again in pairs of fp32 values
 // (two_float.cuh; fp64 took twice as long on this GPU): the candidates alone where that is enough, else the
 // row by way of shared memory.  One such warp sets the time of a small batch (89 rows of 944 experts, softmax

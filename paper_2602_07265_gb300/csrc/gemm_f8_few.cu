@@ -588,7 +588,8 @@ __global__ void __launch_bounds__(kThreads, 1) f8_few_kernel(const __grid_consta
               if (tok0 + j + 1 < t.ntok) dst[static_cast<size_t>(j + 1) * p.N] = static_cast<uint8_t>(two >> 8);
             }
           };
-          if (__any_sync(0xffffffffu, lane < kHalf && F8Divider(s, r).plain))
+          // (Tokens that the tile does not have have the smallest scale, which counts for nothing.)
+          if (__any_sync(0xffffffffu, lane < kHalf && tok0 + lane < t.ntok && F8Divider(s, r).plain))
             quantise([](const F8Divider &div, float a, float b) { return div.slow(a, b); });
           else
             quantise([](const F8Divider &div, float a, float b) { return div(a, b); });
